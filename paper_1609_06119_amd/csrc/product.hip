@@ -976,7 +976,9 @@ int fbdt_packed_weight_grad(const void *dy, int64_t lddy, int64_t m, int32_t n, 
         typedef decltype(t) O;
         hipStream_t s = static_cast<hipStream_t>(stream);
         const __bf16 *y = static_cast<const __bf16 *>(dy);
-        int64_t ldy = lddy;
+        // (a single row may have any stride: the kernel's offsets are those of whole pieces, so
+        // that the rows it has beside this one begin where the buffer's range ends)
+        int64_t ldy = m == 1 ? ceil_div(n, kChunk) * kChunk : lddy;
         if (const int64_t bytes = aligned_rows_bytes(dy, lddy, m, n)) {
             __bf16 *const to = static_cast<__bf16 *>(work);
             ldy = ceil_div(n, kChunk) * kChunk;

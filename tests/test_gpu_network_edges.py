@@ -43,3 +43,28 @@ def test_few_rows_are_exact_on_whole_numbers(m, k, fast):
         b = torch.randint(-2, 3, (n, k), generator=gen(n + k), device=DEV).float()
         got = fb.packed_product(fb.pack(a), fb.pack(b), dtype=F32, fast=fast)
         assert torch.equal(got, a @ b.t())
+
+
+# ---- the weights' gradient of one row -----------------------------------------------
+
+@pytest.mark.parametrize("n", [1, 5, 8, 40, 333])
+@pytest.mark.parametrize("stride", [None, 2 ** 22 + 8, 2 ** 26, 2 ** 31, 2 ** 31 + 8, 2 ** 40 + 24])
+def test_weight_grad_of_one_row_at_any_stride(n, stride):
+    """A single row's stride means nothing: the rows that a step has beside it are no rows,
+    and add nothing to values that are infinite.  NaN lies where they would begin."""
+    from paper_1609_06119_amd._lib import check, lib
+    k = 200
+    wide = torch.full((70 * 340,), float("nan"), dtype=BF16, device=DEV)
+    dy = wide[:n]
+    dy.copy_(normal(n, n, dtype=BF16))
+    dy[n // 2] = float("inf")
+    x = fb.pack(1 + normal(2, 1, k).abs())             # (no zeros: inf * 0 is NaN)
+    out = torch.empty((n, k), device=DEV)
+    L = lib()
+    args = (dy.data_ptr(), n if stride is None else stride, 1, n)
+    assert L.fbdt_packed_weight_grad_work(*args, k) == 0
+    check("fbdt_packed_weight_grad", L.fbdt_packed_weight_grad(
+        *args, x.data.data_ptr(), x.data.shape[1], x.scales.data_ptr(), x.scales.shape[1], k,
+        out.data_ptr(), 0, k, None, 0, torch.cuda.current_stream().cuda_stream))
+    want = R.f64(dy)[:, None] * R.unpack(x)[0]         # 8 + 4 significant bits: exact
+    assert np.array_equal(R.f64(out), want)
