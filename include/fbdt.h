@@ -398,7 +398,7 @@ int fbdt_pack(const void *x, int64_t ldx, int32_t dtype, int64_t n, int32_t widt
  * 8-bit matrix unit, at up to twice the rate: within each group of 8 columns
  * it cuts every product off 2^-13 below the largest one, the groups are added
  * in float32 (about 1.5e-5 of the result's 2-norm on normal data of any width,
- * 8e-5 where values spread over factors of e^4: below a 16-bit result's
+ * 8e-5 with log-normal factors of sigma 2: below a 16-bit result's
  * rounding, but a single result that cancels may be off by more than its own).
  * fast == 0: the values are unpacked
  * to bfloat16, which holds them exactly (but for values below 2^-126, which
