@@ -18,11 +18,13 @@ int report(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)))
 // Compute units of the current device.
 int device_cus(int *cus);
 
+// In an entry of the C ABI.  (Its name stands for the expression, whose text may be a
+// whole function and leave the cause no room in the message.)
 #define NET_TRY(expr)                                                                        \
     do {                                                                                     \
         const hipError_t e_ = (expr);                                                        \
         if (e_ != hipSuccess)                                                                \
-            return report(FBDT_E_DEVICE, "%s failed: %s", #expr, hipGetErrorString(e_));     \
+            return report(FBDT_E_DEVICE, "%s failed: %s", __func__, hipGetErrorString(e_));  \
     } while (0)
 
 // A packed row holds e4m3 codes (largest 448) and one power-of-two scale,
