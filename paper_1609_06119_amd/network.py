@@ -5,9 +5,12 @@ gradient, rows packed in 8 bits, and the products of packed rows with the
 gradient of their weights.
 
 Argument marshalling only, as in api.py: every operator is a kernel of libfbdt
-on the current HIP stream, and all its tensors are on the current device.  Float matrices are float32, bfloat16 or float16
-with unit stride along columns; leading dimensions count as rows where they
-can be viewed as one.
+on the current HIP stream, and all its tensors are on the current device.  Float
+matrices are float32, bfloat16 or float16 with unit stride along columns; leading
+dimensions count as rows where they can be viewed as one.
+
+The calls build no graph of torch's: gradients are calls of their own, and a tensor
+that requires grad is refused while torch records gradients.
 """
 from __future__ import annotations
 
@@ -47,6 +50,9 @@ def _type(t: torch.Tensor, name: str) -> int:
 def _on_gpu(t, name: str):
     at = t.get_device() if isinstance(t, torch.Tensor) else -1      # (-1: on the host)
     if at >= 0 and at == _current_device():
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} requires grad, which the call would not record: call it under "
+                             f"torch.no_grad() and take gradients from the *_grad calls")
         return
     if at < 0:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")

@@ -68,3 +68,36 @@ def test_weight_grad_of_one_row_at_any_stride(n, stride):
         out.data_ptr(), 0, k, None, 0, torch.cuda.current_stream().cuda_stream))
     want = R.f64(dy)[:, None] * R.unpack(x)[0]         # 8 + 4 significant bits: exact
     assert np.array_equal(R.f64(out), want)
+
+
+# ---- gradients that torch would record ------------------------------------------------
+
+def test_tensors_whose_gradient_is_recorded_are_refused():
+    """The calls build no graph: a gradient that torch waits for would be dropped."""
+    x, gain = normal(1, 4, 200), torch.ones(200, device=DEV)
+    t = torch.zeros(4, dtype=torch.int32, device=DEV)
+    p = fb.pack(x)
+    rstd = torch.ones(4, device=DEV)
+    asked, asked_gain, asked_16 = (v.clone().requires_grad_() for v in (x, gain, x.bfloat16()))
+    calls = {
+        "embed": lambda: fb.embed(asked, t), "out": lambda: fb.embed(x, t, out=asked * 1),
+        "embed_grad": lambda: fb.embed_grad(t, asked, 5),
+        "embed_grad of nothing": lambda: fb.embed_grad(t[:0], asked[:0], 5),
+        "rms_norm": lambda: fb.rms_norm(asked, gain), "gain": lambda: fb.rms_norm(x, asked_gain),
+        "residual": lambda: fb.rms_norm(x, gain, residual=asked),
+        "rms_norm_grad": lambda: fb.rms_norm_grad(asked, x, gain, rstd),
+        "dh": lambda: fb.rms_norm_grad(x, x, gain, rstd, dh=asked), "pack": lambda: fb.pack(asked),
+        "product": lambda: fb.packed_product(p, p, dtype=F32, out=asked[:, :4] * 1),
+        "weight_grad": lambda: fb.packed_weight_grad(asked_16, p),
+    }
+    for name, call in calls.items():
+        with pytest.raises(ValueError, match="requires grad"):
+            call()
+            pytest.fail(name)
+        with torch.no_grad():
+            if name not in ("out", "product"):
+                call()
+        with torch.inference_mode():
+            call()
+    with torch.no_grad():
+        assert torch.equal(fb.rms_norm(asked, asked_gain).y, fb.rms_norm(x, gain).y)
