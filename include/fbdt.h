@@ -298,7 +298,9 @@ int fbdt_leaf_values(const uint8_t *node, const int8_t *y, const float *v, const
  *  - Matrices are row-major with a row stride in elements (bytes for codes
  *    and scales); a float matrix may start at any element of its type and
  *    have any stride >= its width, and results may overlay inputs only where
- *    that is said.  All pointers are device pointers.
+ *    that is said (the lookup, its gradient, the tokens and the products refuse
+ *    a result that lies on what they read; columns side by side in one matrix
+ *    are apart).  All pointers are device pointers.
  *  - Packed rows hold 8-bit codes (e4m3: 4 significant bits, largest 448) and
  *    one power-of-two scale for each block of 128 columns, stored as its
  *    biased exponent (e8m0: 2^(byte - 127), 255 = NaN).  Rows of codes are

@@ -969,6 +969,8 @@ int fbdt_event_tokens(const uint8_t *xb, int64_t n, int32_t d, int64_t ldb, int3
     if (n == 0) return FBDT_OK;
     if (!xb || !aligned_to(xb, 16)) return report(FBDT_E_INVAL, "xb must be 16-byte aligned");
     if (!tokens || !aligned_to(tokens, 4)) return report(FBDT_E_INVAL, "tokens must be 4-byte aligned");
+    int rc;
+    if ((rc = check_apart("tokens", {tokens, 1, n * d, 0, 4}, "xb", {xb, d, n, ldb, 1}))) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     event_tokens_kernel<<<grid_of(ceil_div(n, kTokenEvents), kTokenThreads), kTokenThreads,
                           d * kTokenEvents, s>>>(
@@ -985,6 +987,11 @@ int fbdt_embed(const void *table, int32_t dtype, int64_t rows, int32_t width, in
     if ((rc = check_matrix("table", table, dtype, ldt, width))) return rc;
     if (n == 0) return FBDT_OK;
     if ((rc = check_matrix("out", out, dtype, ldo, width))) return rc;
+    const int64_t size = dtype_bytes(dtype);
+    const Extent result = {out, n, width, ldo, size};
+    if ((rc = check_apart("out", result, "table", {table, rows, width, ldt, size})) ||
+        (rc = check_apart("out", result, "tokens", {tokens, 1, n, 0, token_bytes})))
+        return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     NET_TRY(with_dtype(dtype, [&](auto t) {
         typedef decltype(t) T;
@@ -1035,6 +1042,10 @@ int fbdt_embed_grad(const void *tokens, int32_t token_bytes, int64_t n, const vo
     if (work_bytes < p.bytes || (p.bytes > 0 && (!work || !aligned_to(work, 256))))
         return report(FBDT_E_INVAL, "work must hold %lld bytes, 256-byte aligned",
                       (long long)p.bytes);
+    const Extent result = {dtable, rows, width, ldg, dtype_bytes(grad_dtype)};
+    if ((rc = check_apart("dtable", result, "dout", {dout, n, width, ldd, dtype_bytes(dtype)})) ||
+        (rc = check_apart("dtable", result, "tokens", {tokens, 1, n, 0, token_bytes})))
+        return rc;
     int cus = 0;
     if ((rc = device_cus(&cus))) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);

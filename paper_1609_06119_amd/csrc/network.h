@@ -41,6 +41,34 @@ inline bool aligned_to(const void *p, uintptr_t a) {
 }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// `rows` rows of `width` elements of `size` bytes, `stride` elements apart.
+struct Extent {
+    const void *p;
+    int64_t rows, width, stride, size;
+};
+
+// Whether two matrices share a byte.  Rows of one stride may lie side by side in a wider
+// matrix, a single row between the rows of another; rows of two strides that lie among
+// each other are taken to meet.
+inline bool overlap(const Extent &a, const Extent &b) {
+    if (a.rows < 1 || b.rows < 1) return false;
+    typedef __int128 wide;
+    const wide aw = (wide)a.width * a.size, bw = (wide)b.width * b.size;
+    const wide as = (wide)a.stride * a.size, bs = (wide)b.stride * b.size;
+    const wide a0 = (wide)reinterpret_cast<uintptr_t>(a.p), b0 = (wide)reinterpret_cast<uintptr_t>(b.p);
+    if (a0 + (a.rows - 1) * as + aw <= b0 || b0 + (b.rows - 1) * bs + bw <= a0) return false;
+    if (a.rows == 1 && b.rows == 1) return true;
+    if (a.rows > 1 && b.rows > 1 && as != bs) return true;
+    const wide stride = a.rows > 1 ? as : bs;
+    const wide after = ((b0 - a0) % stride + stride) % stride;   // b's columns, from a's on
+    return after < aw || after + bw > stride;
+}
+
+// Refuses a result that lies on what the call reads.
+inline int check_apart(const char *result, const Extent &out, const char *name, const Extent &in) {
+    return overlap(out, in) ? report(FBDT_E_INVAL, "%s overlaps %s", result, name) : FBDT_OK;
+}
+
 // A launch holds fewer than 2^32 threads along x: `groups` workgroups, in rows along y
 // where there are more, and the number of a workgroup among them (of which the last
 // row may have more than `groups`).

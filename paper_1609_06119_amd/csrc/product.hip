@@ -909,6 +909,15 @@ int check_out(void *out, int32_t dtype, int64_t ldo, int64_t n) {
     return FBDT_OK;
 }
 
+// That a result [rows][width] lies apart from packed rows of width k.
+int check_apart_packed(const void *out, int32_t dtype, int64_t rows, int64_t width, int64_t ldo,
+                       const char *name, const Packed &p, int64_t packed_rows, int64_t k) {
+    const Extent result = {out, rows, width, ldo, dtype_bytes(dtype)};
+    const int rc = check_apart("out", result, name, {p.codes, packed_rows, k, p.ld, 1});
+    return rc ? rc : check_apart("out", result, name,
+                                 {p.scales, packed_rows, ceil_div(k, kPackBlock), p.lds, 1});
+}
+
 int check_product(int64_t m, int64_t n, int64_t k) {
     if (m < 0 || m >= (int64_t)1 << 31)
         return report(FBDT_E_INVAL, "m = %lld must be in [0, 2^31)", (long long)m);
@@ -936,9 +945,12 @@ int fbdt_packed_product(const uint8_t *a, int64_t lda, const uint8_t *a_scales, 
     if (m == 0) return FBDT_OK;
     if ((rc = check_packed("a", a, lda, a_scales, ldas, k))) return rc;
     if ((rc = check_out(out, dtype, ldo, n))) return rc;
+    const Packed pa = {a, lda, a_scales, ldas}, pb = {b, ldb, b_scales, ldbs};
+    if ((rc = check_apart_packed(out, dtype, m, n, ldo, "a", pa, m, k)) ||
+        (rc = check_apart_packed(out, dtype, m, n, ldo, "b", pb, n, k)))
+        return rc;
     int cus = 0;
     if ((rc = device_cus(&cus))) return rc;
-    const Packed pa = {a, lda, a_scales, ldas}, pb = {b, ldb, b_scales, ldbs};
     NET_TRY(with_dtype(dtype, [&](auto t) {
         typedef decltype(t) O;
         hipStream_t s = static_cast<hipStream_t>(stream);
@@ -972,6 +984,9 @@ int fbdt_packed_weight_grad(const void *dy, int64_t lddy, int64_t m, int32_t n, 
     if (work_bytes < need || (need > 0 && (!work || !aligned_to(work, 256))))
         return report(FBDT_E_INVAL, "work must hold %lld bytes, 256-byte aligned", (long long)need);
     const Packed px = {x, ldx, x_scales, ldxs};
+    if ((rc = check_apart("out", {out, n, k, ldo, dtype_bytes(dtype)}, "dy", {dy, m, n, lddy, 2})) ||
+        (rc = check_apart_packed(out, dtype, n, k, ldo, "x", px, m, k)))
+        return rc;
     NET_TRY(with_dtype(dtype, [&](auto t) {
         typedef decltype(t) O;
         hipStream_t s = static_cast<hipStream_t>(stream);

@@ -9,6 +9,8 @@ on the current HIP stream, and all its tensors are on the current device.  Float
 matrices are float32, bfloat16 or float16 with unit stride along columns; leading
 dimensions count as rows where they can be viewed as one.
 
+`out`, where a call takes it, must not overlap what the call reads.
+
 The calls build no graph of torch's: gradients are calls of their own, and a tensor
 that requires grad is refused while torch records gradients.
 """

@@ -101,3 +101,26 @@ def test_tensors_whose_gradient_is_recorded_are_refused():
             call()
     with torch.no_grad():
         assert torch.equal(fb.rms_norm(asked, asked_gain).y, fb.rms_norm(x, gain).y)
+
+
+# ---- results beside and on what a call reads --------------------------------------------
+
+def test_results_on_inputs_are_refused_and_beside_them_are_not():
+    wide = normal(1, 60, 100)
+    table = wide[:, :40]
+    t = torch.randint(0, 60, (60,), generator=gen(2), device=DEV)
+    want = table[t]
+    fb.embed(table, t, out=wide[:, 50:90])                     # columns of one matrix
+    assert torch.equal(wide[:, 50:90], want)
+    d = normal(3, 60, 40)
+    a, x = fb.pack(normal(4, 60, 200)), normal(5, 60, 40, dtype=BF16)
+    g = fb.embed_grad(t, d, 60)
+    fb.embed_grad(t, d, 60, out=wide[:, 50:90])
+    assert torch.equal(wide[:, 50:90], g)
+    codes = fb.Codes(torch.zeros((3, 64), dtype=torch.uint8, device=DEV), 10)
+    for call in (lambda: fb.embed(table, t[:30], out=table[:30]), lambda: fb.embed_grad(t, d, 60, out=d),
+                 lambda: fb.event_tokens(codes, 16, out=codes.data.view(torch.int32).view(-1)[:30].view(10, 3)),
+                 lambda: fb.packed_product(a, a, dtype=F32, out=a.data.view(F32)[:, :60]),
+                 lambda: fb.packed_weight_grad(x, a, dtype=BF16, out=torch.as_strided(x, (40, 200), (1, 1)))):
+        with pytest.raises((fb.FbdtError, ValueError), match="overlap"):
+            call()
