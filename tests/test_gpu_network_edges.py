@@ -124,3 +124,53 @@ def test_results_on_inputs_are_refused_and_beside_them_are_not():
                  lambda: fb.packed_weight_grad(x, a, dtype=BF16, out=torch.as_strided(x, (40, 200), (1, 1)))):
         with pytest.raises((fb.FbdtError, ValueError), match="overlap"):
             call()
+
+
+# ---- the norm in place --------------------------------------------------------------------
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+@pytest.mark.parametrize("dtype,code", [(F32, 0), (BF16, 1)])
+@pytest.mark.parametrize("n,width", [(70, 24), (9, 500), (70, 2560), (5, 9000), (5, 28_001), (600, 33_000)])
+@pytest.mark.parametrize("packed", [False, True])
+def test_h_takes_the_place_of_x_or_the_residual(n, width, dtype, code, packed):
+    from paper_1609_06119_amd._lib import check, lib
+    x, r, gain = normal(1, n, width, dtype=dtype), normal(2, n, width, dtype=dtype), normal(3, width)
+    want = fb.rms_norm(x, gain, residual=r, packed=packed)
+    for place in ("x", "residual"):
+        a, b, rstd = x.clone(), r.clone(), torch.empty(n, device=DEV)
+        h = a if place == "x" else b
+        if packed:
+            y = fb.Packed.empty(n, width)
+            to = (None, 0, y.data.data_ptr(), y.data.shape[1], y.scales.data_ptr(), y.scales.shape[1])
+        else:
+            y = torch.empty_like(x)
+            to = (y.data_ptr(), width, None, 0, None, 0)
+        check("fbdt_rms_norm", lib().fbdt_rms_norm(
+            a.data_ptr(), width, b.data_ptr(), width, code, n, width, gain.data_ptr(), 1e-6, h.data_ptr(),
+            width, *to, rstd.data_ptr(), stream()))
+        assert torch.equal(h, want.h) and torch.equal(rstd, want.rstd)
+        assert torch.equal(b if place == "x" else a, r if place == "x" else x)
+        assert torch.equal(y.unpack(), want.y.unpack()) if packed else torch.equal(y, want.y)
+
+
+@pytest.mark.parametrize("dtype,code", [(F32, 0), (BF16, 1)])
+@pytest.mark.parametrize("n,width", [(70, 24), (9, 500), (70, 2560), (70, 4000), (5, 9000), (600, 17_001)])
+def test_dx_takes_the_place_of_dy_or_dh(n, width, dtype, code):
+    from paper_1609_06119_amd._lib import check, lib
+    dy, h, dh = (normal(s, n, width, dtype=dtype) for s in (1, 2, 3))
+    gain, rstd = normal(4, width), 0.5 + normal(5, n).abs()
+    want, want_gain = fb.rms_norm_grad(dy, h, gain, rstd, dh=dh)
+    L = lib()
+    need = L.fbdt_rms_norm_grad_work(n, width)
+    work = torch.empty(need, dtype=torch.uint8, device=DEV)
+    for place in ("dy", "dh"):
+        a, b, dgain = dy.clone(), dh.clone(), torch.empty(width, device=DEV)
+        dx = a if place == "dy" else b
+        check("fbdt_rms_norm_grad", L.fbdt_rms_norm_grad(
+            a.data_ptr(), width, h.data_ptr(), width, b.data_ptr(), width, code, n, width, gain.data_ptr(),
+            rstd.data_ptr(), dx.data_ptr(), width, dgain.data_ptr(), work.data_ptr(), need, stream()))
+        assert torch.equal(dx, want) and torch.equal(dgain, want_gain)
+        assert torch.equal(b if place == "dy" else a, dh if place == "dy" else dy)
