@@ -6,7 +6,7 @@ import torch
 
 import network_ref as R
 import paper_1609_06119_amd as fb
-from test_gpu_network import BF16, DEV, F32, gen, normal
+from test_gpu_network import BF16, DEV, F16, F32, SUM_STEPS, check_packed, gen, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -174,3 +174,39 @@ def test_dx_takes_the_place_of_dy_or_dh(n, width, dtype, code):
             rstd.data_ptr(), dx.data_ptr(), width, dgain.data_ptr(), work.data_ptr(), need, stream()))
         assert torch.equal(dx, want) and torch.equal(dgain, want_gain)
         assert torch.equal(b if place == "dy" else a, dh if place == "dy" else dy)
+
+
+# ---- 8-bit rows ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("width", [4100, 9504, 14_000, 20_000, 24_577, 25_000, 28_672, 32_640, 32_768, 32_769])
+def test_wide_rows_packed(dtype, width):
+    """The codes of rows by 256 lanes to 1024 and of those that are read twice."""
+    x, gain = normal(1, 7, width, dtype=dtype, scale=2.0), 1 + normal(3, width, scale=0.2)
+    x[2] = 0.0
+    p = fb.rms_norm(x, gain, eps=1e-4, packed=True)
+    ry, _, _ = R.rms_norm(R.f64(x), None, R.f64(gain), np.float64(np.float32(1e-4)))
+    check_packed(p.y, ry, (SUM_STEPS + 16) * R.U32)
+    assert not R.f64(p.y.data)[:, width:].any()
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 2, 1), (3, 9, 200), (200, 40, 384), (4100, 300, 130)])
+def test_a_scale_that_is_nan(m, n, k):
+    """It makes its block NaN whatever its codes are, 0 among them, and nothing else."""
+    x, w = fb.pack(1 + normal(1, m, k).abs()), fb.pack(1 + normal(2, n, k).abs())
+    row, block = m // 2, (k - 1) // 128
+    x.scales.view(torch.uint8)[row, block] = 255
+    x.data.view(torch.uint8)[row, 128 * block] = 0
+    nan = np.zeros((m, n), dtype=bool)
+    nan[row] = True
+    for fast in (False, True):
+        assert np.array_equal(np.isnan(R.f64(fb.packed_product(x, w, dtype=F32, fast=fast))), nan)
+        assert np.array_equal(np.isnan(R.f64(fb.packed_product(w, x, dtype=F32, fast=fast))), nan.T)
+    dy = 1 + normal(3, m, n, dtype=BF16).abs()
+    got = R.f64(fb.packed_weight_grad(dy, x))
+    nan = np.zeros((n, k), dtype=bool)
+    nan[:, 128 * block:] = True
+    assert np.array_equal(np.isnan(got), nan)
+    keep = ~nan[0]
+    Y, X = R.f64(dy), R.unpack(x)[0][:, keep]
+    assert (np.abs(got[:, keep] - Y.T @ X) <= (m + 3) * R.U32 * (Y.T @ X)).all()
