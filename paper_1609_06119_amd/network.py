@@ -161,8 +161,8 @@ def _packed(p: Packed, name: str):
                          f"rows of width {width}")
     if rows > 0 and (step != 1 or (sstep != 1 and sheld > 1)):
         raise ValueError(f"{name}: codes and scales must have unit stride along columns")
-    if rows <= 1:
-        ld, lds = held, sheld
+    if rows <= 1:               # (a single row may report any stride)
+        ld, lds = (held + BLOCK - 1) // BLOCK * BLOCK, (sheld + 3) & ~3
     return d.data_ptr(), ld, s.data_ptr(), lds, rows, width
 
 

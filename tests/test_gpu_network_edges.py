@@ -210,3 +210,21 @@ def test_a_scale_that_is_nan(m, n, k):
     keep = ~nan[0]
     Y, X = R.f64(dy), R.unpack(x)[0][:, keep]
     assert (np.abs(got[:, keep] - Y.T @ X) <= (m + 3) * R.U32 * (Y.T @ X)).all()
+
+
+def test_packed_rows_of_one_row():
+    """A row of packed rows is what it is among the others, whatever its tensors hold beside it."""
+    a, b, x = fb.pack(normal(1, 3, 300)), fb.pack(normal(2, 40, 300)), normal(3, 3, 60, dtype=BF16)
+    want = fb.packed_product(a, b, dtype=F32)
+    for held in (384, 300 + 128):
+        for blocks in (3, 4):
+            data = torch.zeros((3, 512), dtype=torch.uint8, device=DEV)
+            data[:, :384] = a.data.view(torch.uint8)
+            scales = torch.zeros((3, 8), dtype=torch.uint8, device=DEV)
+            scales[:, :4] = a.scales.view(torch.uint8)
+            data, scales = data.view(a.data.dtype), scales.view(a.scales.dtype)
+            for rows in (slice(0, 3), slice(1, 2)):
+                p = fb.Packed(data[rows, :held], scales[rows, :blocks], 300)
+                assert torch.equal(fb.packed_product(p, b, dtype=F32), want[rows])
+                got = fb.packed_weight_grad(x[rows], p)
+                assert torch.equal(got, fb.packed_weight_grad(x[rows], fb.pack(p.unpack())))
