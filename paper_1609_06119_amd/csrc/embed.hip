@@ -300,7 +300,8 @@ __device__ __forceinline__ uint32_t rank_in_wave(uint32_t *cnt, uint32_t digit, 
 }
 
 // The pairs of a tile are put in order in LDS first, so that neighbouring lanes
-// write neighbouring places (tiles of 8192, 10M pairs of 128 digits: 54 us, without 110).
+// write neighbouring places (10M pairs of 128 digits: 43 us from the tokens, 35 from sorted
+// keys; in tiles of twice the size 54, and 110 with every pair written from its register).
 template <typename I, bool FIRST, bool FEW>
 __global__ __launch_bounds__(kSortThreads) void digit_scatter_kernel(
     const I *__restrict__ keys, const uint32_t *__restrict__ index, uint32_t n, uint32_t rows,
@@ -852,7 +853,9 @@ hipError_t table_gradient(const GradPlan &p, const void *tokens, int token_bytes
     int at = 0;
     // One workgroup sorts few tokens faster than a launch per step (4000: 33 and 38 us in
     // all; 8000: 40 and 40; 16,000: 52 and 43), and up to kSmallSort of them if the
-    // zeros beside it take as long (16,384 and 268 MB: 102 and 114).
+    // zeros beside it take as long (10,000 tokens and 34 MB of zeros, 50 and 49; 67 MB, 50 and
+    // 55; 134 MB, 57 and 71; 268 MB, 93 and 104; 16,384 and 67 MB, 61 and 57; 134 MB, 73 and
+    // 75; 268 MB, 99 and 111; 537 MB, 157 and 163).
     const bool small = n <= kSmallSort / 2 ||
                        (n <= kSmallSort && rows * width * (int64_t)sizeof(O) >= (int64_t)1 << 27);
     if (n > 0 && small) {
