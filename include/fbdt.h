@@ -396,15 +396,15 @@ int fbdt_pack(const void *x, int64_t ldx, int32_t dtype, int64_t n, int32_t widt
  * in float32 and rounded once to `dtype`.  a: m packed rows of width k
  * (activations, or a gradient); b: n packed rows of width k (weights); out:
  * [m][n].  m may be 0; n, k <= 2^20, and at most 2^31 tiles of 16 x 16 in m x
- * n.  fast != 0: the products are added by the
- * 8-bit matrix unit, at up to twice the rate: within each group of 8 columns
+ * n.  fast != 0: products of more than a few rows may be added by the 8-bit
+ * matrix unit, at about twice the rate: within each group of 8 columns
  * it cuts every product off 2^-13 below the largest one, the groups are added
  * in float32 (about 1.5e-5 of the result's 2-norm on normal data of any width,
  * 8e-5 with log-normal factors of sigma 2: below a 16-bit result's
  * rounding, but a single result that cancels may be off by more than its own).
- * fast == 0: the values are unpacked
- * to bfloat16, which holds them exactly (but for values below 2^-126, which
- * may count as 0), and every product is added in full.
+ * fast == 0, and up to 8 rows: the values are unpacked to bfloat16, which holds
+ * them exactly (but for values below 2^-126, which may count as 0), and every
+ * product is added in full.
  */
 int fbdt_packed_product(const uint8_t *a, int64_t lda, const uint8_t *a_scales, int64_t ldas,
                         int64_t m, const uint8_t *b, int64_t ldb, const uint8_t *b_scales,

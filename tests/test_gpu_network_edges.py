@@ -228,3 +228,13 @@ def test_packed_rows_of_one_row():
                 assert torch.equal(fb.packed_product(p, b, dtype=F32), want[rows])
                 got = fb.packed_weight_grad(x[rows], p)
                 assert torch.equal(got, fb.packed_weight_grad(x[rows], fb.pack(p.unpack())))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,n,k", [(1, 10_240, 2560), (1, 40, 9000), (5, 1280, 1280), (8, 777, 1300),
+                                   (16, 500, 640)])
+def test_few_rows_are_added_in_full(m, n, k, dtype):
+    """The 8-bit unit's sums would save them next to nothing: fast gives the same bits."""
+    a, b = fb.pack(normal(m, m, k)), fb.pack(normal(n, n, k))
+    want = fb.packed_product(a, b, dtype=dtype)
+    assert torch.equal(fb.packed_product(a, b, dtype=dtype, fast=True), want)
