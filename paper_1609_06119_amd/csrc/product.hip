@@ -543,8 +543,10 @@ hipError_t launch_tiles(const Packed &a, const Packed &b, int64_t m, int64_t n, 
 // 14.6 and 17.3; 3000 x 5000 x 700 34, 26 and 32; 128 x 10,240 x 2560 28, 13.9 and 11.2.
 // Few rows take the kernel for them (weights from memory: one row times 10,240 x 2560 8.8 us,
 // by tiles with fast sums 18.2; times 1280 x 1280 3.8 and 7.5; times 20,480 x 8192 35 and 55;
-// 8 rows times 5120 x 5120 11.8 and 32; 16 rows times 512 x 9000 11.5 and 37), but 16 rows
-// times 10,240 x 2560 in cache took 10.2 and 8.6: the workgroups read more of a than of b.  Sums in full take the 128 x 128 tile where they would take the largest one,
+// 8 rows times 5120 x 5120 11.8 and 32; 16 rows times 512 x 9000 11.5 and 37).  9 to 16
+// rows times many take tiles: 16 times 10,240 x 2560 with weights in cache 8.4, by the other
+// 9.7, times 40,000 x 640 6.7 and 12, as the workgroups read more of a than of b (weights
+// from memory: 18.2 and 11.4, 9.1 and 13.4).  Sums in full take the 128 x 128 tile where they would take the largest one,
 // whose unpacked fragments leave too few registers.
 //
 // Workgroups that take tile after tile are as many as run at a time: 65,536 x 1280 x 1280

@@ -324,10 +324,10 @@ def packed_product(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16,
                    out: torch.Tensor | None = None, fast: bool = False) -> torch.Tensor:
     """a b^T, [a.rows][b.rows]: activations (or a gradient) times weights, both packed
     along the width that is summed; added in float32 and rounded once.  fast: more than
-    a few rows are added by the 8-bit matrix unit, about twice as fast, to about 1.5e-5 of the result's norm on
-    normal data (products are cut off 2^-13 below the largest of their group of 8): enough
-    for a 16-bit result, though a single one that cancels may be off by more than its
-    own rounding."""
+    a few rows are added by the 8-bit matrix unit, about twice as fast, to about 1.5e-5 of
+    the result's norm on normal data (products are cut off 2^-13 below the largest of
+    their group of 8): enough for a 16-bit result, though a single one that cancels may be
+    off by more than its own rounding."""
     pa, lda, sa, ldsa, m, k = _packed(a, "a")
     pb, ldb, sb, ldsb, n, kb = _packed(b, "b")
     if k != kb:
